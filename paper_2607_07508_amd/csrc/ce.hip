@@ -137,16 +137,18 @@ struct EpiExp {
   __device__ __forceinline__ void finish(int, int64_t, int, int, int, void*) {}
 };
 
-// Up to two token tiles the products are bound by reading W, each of its tiles by one or two workgroups, and these
-// start K at slabs of their own: rows 2 H bytes apart make workgroups in step read from the same memory channels
+// Up to two token tiles the products are bound by reading W, each of its tiles by one or two workgroups, and vocabulary
+// tiles start K at slabs of their own: rows 2 H bytes apart make workgroups in step read from the same memory channels
 // (256 rows of 2048 x 151,936 264 -> 219 us, of 6144 695 -> 570; 300 of 6144 914 -> 825). With more token tiles
 // the workgroups that share a tile of W keep in step, in a kernel without the wrap (4096 rows: 2055 us, 2102 with).
 constexpr int kRotateMaxTokenTiles = 2;
+// XCD x takes tiles x, x + 8, ..., its workgroups in turn: slab i + 4 x for the i-th of them.
+__device__ __forceinline__ int rotated_slab(int mt, int nk) {
+  return static_cast<int>((static_cast<unsigned>(mt) / 8 + 4 * (static_cast<unsigned>(mt) & 7)) % static_cast<unsigned>(nk));
+}
 struct PlainTiles : PullTiles {};
 struct RotatedTiles : PullTiles {
-  __device__ __forceinline__ int first_slab(int nk) const {
-    return static_cast<int>(((blockIdx.x >> 3) / nv + 4 * (blockIdx.x & 7)) % static_cast<unsigned>(nk));
-  }
+  __device__ __forceinline__ int first_slab(int mt, int nk) const { return rotated_slab(mt, nk); }
 };
 // The tiles are pulled per XCD from its list (PullTiles), those of a partial last vocabulary tile
 // (st.m > 0) after the whole ones, which stream. Bound by the MFMAs under the power limit: 4178 rows of 2048 x
@@ -396,16 +398,17 @@ static __global__ __launch_bounds__(64) void k_chunk_counts(const int32_t* count
 // The rows that count gathered into hc, zero-filled up to a whole token tile (the first gather_blocks
 // blocks), and, for the cross entropy, the targets' logits zt[c] = h_c . W[y_c] (the others). For bf16 four rows
 // a wave on MFMA, of which the diagonal is kept: the same products in the same order as in the logits' tiles, so
-// that zt equals the term in the sum (where the tiles do not wrap K, to the last bit) and 1 - p keeps its digits
-// when p is nearly 1. For fp32 one row a wave; there p comes from the stored exponential. Targets outside [0, V):
-// nothing reads their zt.
+// that zt equals the term in the sum to the last bit and 1 - p keeps its digits when p is nearly 1. Targets in the
+// first rotated_tiles vocabulary tiles start K where those do. For fp32 one row a wave; there p comes from the stored
+// exponential. Targets outside [0, V): nothing reads their zt.
 template <class E>
 constexpr int kDotRows = sizeof(typename E::storage) == 2 ? 4 : 1;
 template <class E>
 __global__ __launch_bounds__(256) void k_gather_dots(const typename E::storage* src, int64_t ld_src, int64_t H,
                                                      const int32_t* idx, const int32_t* count, int64_t gather_blocks,
                                                      typename E::storage* hc, const typename E::storage* w, int64_t ld_w,
-                                                     int64_t V, const int32_t* target, float* zt) {
+                                                     int64_t V, const int32_t* target, int64_t rotated_tiles,
+                                                     float* zt) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n = *count;
   const int64_t chunks = H / E::kPerChunk;
@@ -427,10 +430,13 @@ __global__ __launch_bounds__(256) void k_gather_dots(const typename E::storage* 
     __shared__ v4u s_rows[4][8][kPitch];
     v4u(*sh)[kPitch] = s_rows[wave];
     const v4u* row[8];
+    int64_t start[4];  // chunk of row i that comes first
+    const int slabs = static_cast<int>(chunks / kRowChunks);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int64_t t = idx[c0 + i < n ? c0 + i : n - 1];
       const int32_t y = target[t];
+      start[i] = y >= 0 && y / kBM < rotated_tiles ? kRowChunks * rotated_slab(y / kBM, slabs) : 0;
       row[i] = reinterpret_cast<const v4u*>(w + (y >= 0 && y < V ? static_cast<int64_t>(y) : 0) * ld_w);
       row[4 + i] = reinterpret_cast<const v4u*>(src + t * ld_src);
     }
@@ -439,7 +445,10 @@ __global__ __launch_bounds__(256) void k_gather_dots(const typename E::storage* 
     v4u next[8];
     auto load = [&](int64_t k) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) next[i] = k + lane < chunks ? row[i][k + lane] : zero4();
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = k + lane + start[i & 3];
+        next[i] = k + lane < chunks ? row[i][at < chunks ? at : at - chunks] : zero4();
+      }
     };
     load(0);
     for (int64_t k = 0; k < chunks; k += kSpan) {
@@ -1247,6 +1256,12 @@ inline bool few_f32(int64_t rows, int64_t T, int64_t H, int64_t V, const HeadLos
 }
 constexpr int64_t kDhFewRows = 64, kDwFewRowsF32 = 32;
 
+// Whether whole vocabulary tiles start K at slabs of their own: few token tiles, and no slab that K ends inside.
+template <class E>
+static bool rotates(const HeadLossLayout& L, int64_t H) {
+  return L.rows / kTile <= kRotateMaxTokenTiles && H % (kRowChunks * E::kPerChunk) == 0;
+}
+
 template <class E, bool kStore>
 static void launch_exp_logits(const HeadLossArgs& a, const HeadLossLayout& L, const typename E::storage* hc,
                               const int32_t* rows, float2* part, typename E::storage* ex, const int32_t* idx,
@@ -1276,8 +1291,7 @@ static void launch_exp_logits(const HeadLossArgs& a, const HeadLossLayout& L, co
   }
   EpiExp<E, false, kStore> e{ex, L.ldv, part, L.rows, full, 0, scale};
   EpiExp<E, true, kStore> et{ex, L.ldv, part, L.rows, a.V - full, full / kBM, scale};
-  const auto kernel = s.n_tiles <= kRotateMaxTokenTiles ? k_exp_logits<E, kStore, RotatedTiles>
-                                                        : k_exp_logits<E, kStore, PlainTiles>;
+  const auto kernel = rotates<E>(L, a.H) ? k_exp_logits<E, kStore, RotatedTiles> : k_exp_logits<E, kStore, PlainTiles>;
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pull_grid())), dim3(kThreads), 0, st, s, tail, e, et, next);
 }
 
@@ -1319,7 +1333,7 @@ static hipError_t head_loss(const HeadLossArgs& a, hipStream_t st) {
   const int64_t dot_blocks = distill || few_logits ? 0 : ceil_div(a.T, 4 * kDotRows<E>);
   hipLaunchKernelGGL(k_gather_dots<E>, dim3(rows4 + static_cast<unsigned>(dot_blocks)), dim3(256), 0, st,
                      static_cast<const S*>(a.hidden), a.ld_hidden, a.H, idx, count, static_cast<int64_t>(rows4), hc, w,
-                     a.ld_w, a.V, a.ids, zt);
+                     a.ld_w, a.V, a.ids, rotates<E>(L, a.H) ? a.V / kBM : 0, zt);
   if (distill)
     hipLaunchKernelGGL(k_target_dots<E>, dim3(rows4, static_cast<unsigned>(ceil_div(K, kIds))), dim3(256), 0, st, hc, a.H,
                        w, a.ld_w, a.V, idx, a.ids, a.ld_ids, K, count, 1.0f / a.tau, zt, a.status);

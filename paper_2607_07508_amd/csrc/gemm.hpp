@@ -595,11 +595,12 @@ __device__ __forceinline__ void gemm_tile(const GemmShape& s, Epi& epi, v4u (*ld
 struct OneTile {
   static constexpr bool kStream = false;
 };
-// Tiles may have first_slab(nk): the slab of K that a workgroup starts with, wrapping around.
+// Tiles may have first_slab(mt, nk): the slab of K that tile row mt's sums start with, wrapping around. By the tile
+// alone, whichever workgroup takes it, so that the order of a sum never depends on who comes first.
 template <class Tiles, class = void>
 struct HasFirstSlab : std::false_type {};
 template <class Tiles>
-struct HasFirstSlab<Tiles, std::void_t<decltype(std::declval<Tiles&>().first_slab(0))>> : std::true_type {};
+struct HasFirstSlab<Tiles, std::void_t<decltype(std::declval<Tiles&>().first_slab(0, 0))>> : std::true_type {};
 
 // The generic kernel body: one 256 x 256 tile per workgroup. Epi provides:
 //   begin(n0, wm, wn, lane)                 before the K loop
@@ -732,7 +733,10 @@ __device__ __forceinline__ void gemm_tiles(const GemmShape& s, Epi& epi, v4u (*l
   const bool tail = k_valid < static_cast<int64_t>(nk) * G::kRows;
   constexpr bool kRotate = HasFirstSlab<std::remove_reference_t<Tiles>>::value;
   int first = 0;
-  if constexpr (kRotate) first = tail ? 0 : tiles.first_slab(nk);
+  auto start_slab = [&](int tile_row) {
+    if constexpr (kRotate) first = tail ? 0 : tiles.first_slab(tile_row, nk);
+  };
+  start_slab(mt);
   // Scalar base address of slab kt of operand A or B (the slab's offset is
   // uniform and goes into the base; the lanes' offsets stay fixed).
   auto slab_ptr = [&](bool is_a, int kt) -> const char* {
@@ -963,6 +967,7 @@ __device__ __forceinline__ void gemm_tiles(const GemmShape& s, Epi& epi, v4u (*l
       n0 = static_cast<int64_t>(n_tile) * kBN;
       a_base = static_cast<const char*>(s.a) + m0 * s.lda * esz;
       b_base = static_cast<const char*>(s.b) + n0 * s.ldb * esz;
+      start_slab(mt);
       copy_first();
     }
     epi.tile(acc, factor, m_done, n_done, wm, wn, lane, tiles.scratch());
