@@ -441,7 +441,8 @@ sao_status_t sao_value_loss_store(const void* hidden, int64_t ld_hidden, const v
  * logit, up to 5 GiB: three products of tokens x H x V in all. V x element size may span at most 2^24
  * bytes, as any row stride. A target outside [0, V) of a token that counts sets SAO_STATUS_TARGET_RANGE and
  * makes its nll, its dhidden row, dw_head and loss NaN; a log-sum-exp that is not finite sets
- * SAO_STATUS_NONFINITE. Reductions run in a fixed order.
+ * SAO_STATUS_NONFINITE. So does one of magnitude 1.8e8 or more (bf16; 7.4e8 for float32), where float32 logits
+ * lie 16 (64) apart: that token's outputs, dw_head and loss are NaN. Reductions run in a fixed order.
  * ws: sao_head_loss_workspace_size(T, H, V, 1, dtype, out, dhidden != NULL, dw_head != NULL) bytes.
  */
 sao_status_t sao_cross_entropy(const void* hidden, int64_t ld_hidden, const void* w_head, int64_t ld_w,

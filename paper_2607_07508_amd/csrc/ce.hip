@@ -19,8 +19,9 @@
 // 2^15: 11 significand bits down to 2^-29 of it, an absolute 2^-39 of it below. dz is rounded once more,
 // to bf16, whose 8 bits dominate; lse and the loss come from the unrounded sums. The mean's 1 / N (and tau)
 // multiply the gradients' sums: in dz they would be rounded alike in every token whose p is small against 1,
-// as much as 2^-8 off in all of them. Referring to the half tile's own maximum keeps every finite logit in
-// range without a row maximum known beforehand.
+// as much as 2^-8 off in all of them. Referring to the half tile's own maximum keeps logits in range without a
+// row maximum known beforehand: of magnitudes up to 1.8e8 (kMaxRef), where float32 logits lie 16 apart; rows whose
+// log-sum-exp is beyond that are NaN and flagged, halves beyond it below their row's largest are 0.
 #include "common.hpp"
 #include "head.hpp"
 #include "launch.hpp"
@@ -34,6 +35,26 @@ constexpr float kLn2 = 0.6931471805599453f;
 // log2 of the scale of the stored exponentials.
 template <class E>
 constexpr float kExpShift = sizeof(typename E::storage) == 2 ? 15.0f : 0.0f;
+// The largest log-sum-exp of a row, in log2 units. Below it a reference's spacing is 16 for bf16 (64 for fp32), so a
+// half's largest exponential is stored as at least 2^-0.5 (2^-63.5): within fp16, and ahead of what underflows.
+template <class E>
+constexpr float kMaxRef = sizeof(typename E::storage) == 2 ? 0x1p28f : 0x1p30f;
+
+// The reference of a half tile with maximum `top`: sc top less the shift, as a float; the exponents' distances from it
+// are exact up to their own rounding. From 2^24 on its rounding is of the shift's size and would take the largest
+// exponential out of fp16: there it is the float above. A half without a logit above -inf is taken relative to 0, one
+// whose reference would be below every float relative to the lowest (its exponentials are 0).
+template <class E>
+__device__ __forceinline__ float half_reference(float top, float sc) {
+  if (top == -__builtin_inff()) return 0.0f;
+  const float ref = fmaxf(fmaf(top, sc, -kExpShift<E>), -__FLT_MAX__);
+  if (fmaf(top, sc, -ref) > kExpShift<E> + 0.5f) return __uint_as_float(__float_as_uint(ref) + (ref > 0.0f ? 1u : ~0u));
+  return ref;
+}
+// Its pair: of a half without a logit above -inf (-inf, 0) unless a NaN is among them.
+__device__ __forceinline__ float2 half_pair(float top, float ref, float s) {
+  return make_float2(top == -__builtin_inff() && s == 0.0f ? -__builtin_inff() : ref, s);
+}
 
 // ------------------------------------------------------------------------- //
 // (A) logits, exponentials and their sums
@@ -91,10 +112,7 @@ struct EpiExp {
 #pragma unroll
       for (int i = 0; i < kMI * 16; ++i) top = fmaxf(top, z[i]);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      // The reference: the half's maximum less the shift, as a float; the exponents' distances from it are
-      // exact up to their own rounding. A half without a logit above -inf is taken relative to 0, and its
-      // pair is (-inf, 0) unless a NaN is among them.
-      const float ref = top == -__builtin_inff() ? 0.0f : fmaf(top, sc, -kExpShift<E>);
+      const float ref = half_reference<E>(top, sc);
       float s = 0.0f;
 #pragma unroll
       for (int i = 0; i < kMI * 16; ++i) {
@@ -103,7 +121,7 @@ struct EpiExp {
       }
       s += __shfl_xor(s, 32, 64);
       if (lane < 32)
-        part[(2 * (tile0 + m0 / kBM) + wm) * ldp + col] = make_float2(s == 0.0f ? -__builtin_inff() : ref, s);
+        part[(2 * (tile0 + m0 / kBM) + wm) * ldp + col] = half_pair(top, ref, s);
       if constexpr (kStore) {
         typename E::storage* row = ex + col * lde + (tile0 * kBM + m0 + wm * (kBM / 2));
         if constexpr (sizeof(typename E::storage) == 2) {
@@ -350,7 +368,7 @@ __global__ __launch_bounds__(256) void k_exp_logits_few(const typename E::storag
   for (int t = 0; t < NT; ++t) {
     const int tok = t * 16 + r16;
     const float top = fmaxf(fmaxf(s_top[0][tok], s_top[1][tok]), fmaxf(s_top[2][tok], s_top[3][tok]));
-    const float ref = top == -__builtin_inff() ? 0.0f : fmaf(top, scale, -kExpShift<E>);  // as in EpiExp
+    const float ref = half_reference<E>(top, scale);
     float s = 0.0f;
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
@@ -378,8 +396,7 @@ __global__ __launch_bounds__(256) void k_exp_logits_few(const typename E::storag
   if (tid < kTokens && tid < n) {
     const float top = fmaxf(fmaxf(s_top[0][tid], s_top[1][tid]), fmaxf(s_top[2][tid], s_top[3][tid]));
     const float s = (s_sum[0][tid] + s_sum[1][tid]) + (s_sum[2][tid] + s_sum[3][tid]);
-    const float ref = top == -__builtin_inff() ? 0.0f : fmaf(top, scale, -kExpShift<E>);
-    part[static_cast<int64_t>(blockIdx.x) * ldp + tid] = make_float2(s == 0.0f ? -__builtin_inff() : ref, s);
+    part[static_cast<int64_t>(blockIdx.x) * ldp + tid] = half_pair(top, half_reference<E>(top, scale), s);
   }
 }
 
@@ -552,7 +569,9 @@ struct LossRows {
   const float* teacher_lse;
   float tau, z_coef;
   float scale_z;            // log2(e), zt being logits / tau
-  const float* ex;          // fp32 operands: the stored exponentials, row stride lde; else null
+  float max_ref;            // of a row that is not out of range
+  const void* ex;           // the stored exponentials, row stride lde, fp16 or (f32) fp32
+  bool f32;
   int64_t lde;
   float* token_loss;
   float* lse;
@@ -575,11 +594,16 @@ struct RowLse {
 
 // p at vocabulary row v, whose logit by a separate product is z. fp32: of the stored exponential, which the
 // sum holds to the last bit; from z it would differ by a rounding, half as much again as the gradient's error
-// without it.
+// without it. bf16: from z, which has more digits than the stored one, and for the cross entropy is the term in the sum
+// itself. The distillation's differs from it by some 2^-23 of its size, from |z| of 2^12 on (log2 units) more
+// than the 2^-11 that the stored one is rounded by, which is taken there.
+template <bool kDistill>
 __device__ __forceinline__ float sparse_p(const LossRows& a, const RowLse& l, int64_t r, int32_t v, float z) {
-  if (a.ex)
-    return a.ex[r * a.lde + v] * fast_exp2(a.part[static_cast<int64_t>(v / kHalfTile) * a.ldp + r].x - l.ref) / l.sum;
-  return fast_exp2(fmaf(z, a.scale_z, -l.ref)) / l.sum;
+  const bool stored = a.f32 || (kDistill && fabsf(l.ref) >= 4096.0f);
+  if (!stored) return fast_exp2(fmaf(z, a.scale_z, -l.ref)) / l.sum;
+  const int64_t at = r * a.lde + v;
+  const float e = a.f32 ? static_cast<const float*>(a.ex)[at] : static_cast<float>(static_cast<const _Float16*>(a.ex)[at]);
+  return e * fast_exp2(a.part[static_cast<int64_t>(v / kHalfTile) * a.ldp + r].x - l.ref) / l.sum;
 }
 
 // Cross entropy: c = weight / N, loss c (lse - z_y) and z_coef c lse^2,
@@ -599,7 +623,7 @@ __device__ __forceinline__ void ce_row(const LossRows& a, int64_t r, int64_t t, 
   sum[1] += static_cast<double>(c) * a.z_coef * lse * lse;
   if (a.patch) {
     // a target outside the vocabulary makes the whole row's gradient NaN
-    const float p = ok ? sparse_p(a, l, r, y, z) : 0.0f;
+    const float p = ok ? sparse_p<false>(a, l, r, y, z) : 0.0f;
     a.scale[r] = ok ? weight * (1.0f + zl) / l.sum : __builtin_nanf("");
     a.patch[r] = weight * ((p - 1.0f) + zl * p);
   }
@@ -663,7 +687,7 @@ __device__ __forceinline__ void distill_row(const LossRows& a, int64_t r, int64_
     const int32_t id = s_id[k];
     float qs = 0.0f;
     for (int i = 0; i < a.K; ++i) qs += s_id[i] == id ? s_q[i] : 0.0f;
-    const float p = id >= 0 && id < a.V ? sparse_p(a, l, r, id, a.zt[r * a.K + k]) : 0.0f;
+    const float p = id >= 0 && id < a.V ? sparse_p<true>(a, l, r, id, a.zt[r * a.K + k]) : 0.0f;
     a.patch[r * a.K + k] = weight * (Q * p - qs);
   }
 }
@@ -721,7 +745,8 @@ __global__ __launch_bounds__(256) void k_loss_rows(LossRows a) {
     float m = s_ms[0][tid].x, s = s_ms[0][tid].y;
 #pragma unroll
     for (int q = 1; q < 4; ++q) merge(m, s, s_ms[q][tid].x, s_ms[q][tid].y);
-    const RowLse l{m, s};
+    // (-inf stays: a row without a logit above it)
+    const RowLse l{m, fabsf(m) >= a.max_ref && m != -__builtin_inff() ? __builtin_nanf("") : s};
     s_lse[tid] = l;
     if (r0 + tid < n) {
       if (a.patch) a.ref[r0 + tid] = m;
@@ -1368,7 +1393,9 @@ static hipError_t head_loss(const HeadLossArgs& a, hipStream_t st) {
     r.tau = a.tau;
     r.z_coef = a.z_coef;
     r.scale_z = kLog2e;
-    r.ex = k16 ? nullptr : reinterpret_cast<const float*>(ex);
+    r.max_ref = kMaxRef<E>;
+    r.ex = ex;
+    r.f32 = !k16;
     r.lde = L.ldv;
     r.token_loss = a.token_loss;
     r.lse = a.lse;
