@@ -275,7 +275,8 @@ __device__ __forceinline__ double balance_rows(const BalanceArgs& a, const Balan
         read_f();
       }
       // p = w / S with w = e^(x - top), or sigmoid(x) e^(-top), top = min(max x, 0): neither over- nor
-      // underflows where x is far below 0. slope = 1 - sigmoid(x).
+      // underflows where x is far below 0. slope = 1 - sigmoid(x). The difference comes before the factor of
+      // log2 e, which would take the type's largest and lowest values (masked experts) out of float32.
       float top = -__builtin_inff();
 #pragma unroll
       for (int i = 0; i < ITER; ++i)
@@ -285,7 +286,6 @@ __device__ __forceinline__ double balance_rows(const BalanceArgs& a, const Balan
       if (kSigmoid) top = fminf(top, 0.0f);
       // Where top is 0 for every token of the wave, as almost always, e^(min(x, 0) - top) is 1 or e^-|x|.
       const bool shifted = kSigmoid && __ballot(top != 0.0f) != 0;
-      const float top2 = top * kLog2e;
       float slope[ITER][VEC];
       float s = 0.0f, d = 0.0f;
 #pragma unroll
@@ -301,7 +301,7 @@ __device__ __forceinline__ double balance_rows(const BalanceArgs& a, const Balan
             if (shifted) p = fast_exp2((fminf(v, 0.0f) - top) * kLog2e) * r;
             slope[i][j] = (v > 0.0f ? q : 1.0f) * r;
           } else {
-            p = fast_exp2(fmaf(v, kLog2e, -top2));
+            p = fast_exp2((v - top) * kLog2e);
             slope[i][j] = 1.0f;
           }
           x[g][i][j] = p;
