@@ -284,8 +284,8 @@ __device__ __forceinline__ double balance_rows(const BalanceArgs& a, const Balan
         for (int j = 0; j < VEC; ++j) top = fmaxf(top, x[g][i][j]);
       top = lanes_max<LANES>(top);
       if (kSigmoid) top = fminf(top, 0.0f);
-      // Where top is 0 for every token of the wave, as almost always, e^(min(x, 0) - top) is 1 or e^-|x|.
-      const bool shifted = kSigmoid && __ballot(top != 0.0f) != 0;
+      // Where top is 0 for every token of the wave that counts, as almost always, e^(min(x, 0) - top) is 1 or e^-|x|.
+      const bool shifted = kSigmoid && __ballot(on[g] && top != 0.0f) != 0;
       float slope[ITER][VEC];
       float s = 0.0f, d = 0.0f;
 #pragma unroll

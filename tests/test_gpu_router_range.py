@@ -47,3 +47,20 @@ def test_rows_of_extreme_values(T, E, dtype, score):
     # p (f - sum f p): the difference's terms are at most the largest f
     size = E * ref["counts"].max() / (k * T) / T
     assert (np.abs(got - want) <= 1e-5 * size + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T,E", [(60, 64), (4000, 64)])
+def test_masked_neighbours_do_not_matter(T, E, score):
+    """Tokens that count get the same gradient, to the last bit, whatever the masked tokens beside them hold."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn((T, E), generator=g, device="cuda")
+    ids = torch.topk(x, 4, dim=1).indices.to(torch.int32)
+    m = (torch.rand(T, generator=g, device="cuda") < 0.6).to(torch.uint8)
+    off = m == 0
+    first = [v.clone() for v in sao.balance_loss(x, ids, m, score=score)]
+    assert not first[2][off].any()
+    for value in (-500.0, 500.0, float("-inf"), float("nan")):
+        other = x.clone()
+        other[off] = value
+        assert all(torch.equal(a, b) for a, b in zip(first, sao.balance_loss(other, ids, m, score=score)))
