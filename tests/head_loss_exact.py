@@ -29,12 +29,13 @@ def head_loss(h, w, c, target=None, ids=None, teacher=None, tau=1.0, z_coef=0.0)
         a = 1.0 + 2.0 * z_coef * lse
     else:
         u = torch.where(ids >= 0, teacher.double() / tau, -torch.inf)
-        logq = torch.log_softmax(u, 1)
+        some = (u > -torch.inf).any(1, keepdim=True)   # a row without an entry: q = 0
+        logq = torch.where(some, torch.log_softmax(u, 1), -torch.inf)
         qk = torch.exp(logq)
         at = ids.long().clamp(min=0)
         q.scatter_add_(1, at, qk)
         token = tau ** 2 * torch.where(qk > 0, qk * (logq - z.gather(1, at) + lse), 0.0).sum(1, keepdim=True)
-        a = 1.0
+        a = qk.sum(1, keepdim=True)
     out = dict(token=(token * on)[:, 0], lse=(lse * on)[:, 0], z=float(z.abs().max()))
     dz = c * tau * (a * p - q)
     both = c * tau * (a * p + q)
