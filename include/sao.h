@@ -438,7 +438,8 @@ sao_status_t sao_value_loss_store(const void* hidden, int64_t ld_hidden, const v
  * added to or written. z_coef must be finite and >= 0.
  * Neither the logits nor, without a gradient, anything of size T x V reaches memory. For the gradient the
  * tokens that count pass through in chunks, whose exponentials lie in ws at 2 bytes (bf16) or 4 (fp32) per
- * logit, up to 5 GiB: three products of tokens x H x V in all. V x element size may span at most 2^24
+ * logit, up to 5 GiB: three products of tokens x H x V in all. With bf16 operands dz is rounded to bf16 before the
+ * products of the gradients, whatever dw_head's type. V x element size may span at most 2^24
  * bytes, as any row stride. A target outside [0, V) of a token that counts sets SAO_STATUS_TARGET_RANGE and
  * makes its nll, its dhidden row, dw_head and loss NaN; a log-sum-exp that is not finite sets
  * SAO_STATUS_NONFINITE. So does one of magnitude 1.8e8 or more (bf16; 7.4e8 for float32), where float32 logits
@@ -464,7 +465,10 @@ sao_status_t sao_cross_entropy(const void* hidden, int64_t ld_hidden, const void
  *   token_loss[t] = tau^2 sum_k q_k (log q_k - (z_{id_k} - lse[t]))   (0 where mask is 0; overwritten)
  *   loss[0]      += sum_t c_t token_loss[t]
  *   dz_{t,v}      = c_t tau ((sum_k q_k) p_v - sum_{k: id_k = v} q_k)
- * and dhidden, dw_head, mask, weight, N, lse, loss (float64 [1]) and `out` as for sao_cross_entropy. An id of
+ * and dhidden, dw_head, mask, weight, N, lse, loss (float64 [1]) and `out` as for sao_cross_entropy. With Q =
+ * sum_k q_k the sum is Q KL(q / Q || p) + Q log Q: teacher_lse weighs a token by the part Q of the teacher's
+ * probability that its K entries hold, and the optimum is the teacher renormalised over them, not the teacher; where p
+ * is the teacher's own softmax the gradient is not 0. An id of
  * -1 is no entry (its logit is not used), so rows may hold fewer than K; a row without any contributes 0. A
  * logit of -inf contributes 0. An id that occurs twice counts with the sum of its q. Other ids outside
  * [0, V) set SAO_STATUS_TARGET_RANGE and make that token's outputs, dw_head and loss NaN. tau must be finite

@@ -621,7 +621,8 @@ def cross_entropy(hidden: torch.Tensor, w_head: torch.Tensor, target: torch.Tens
 
     loss is {token mean of nll, z_coef times that of lse^2}. dhidden [T, H] is in hidden's dtype and dw_head
     [V, H] in w_head's; each is None if not wanted. With `loss` or `dw_head` (float32) given, the call adds to
-    them instead, as chunks of a batch do (give both, and the batch's n_tokens)."""
+    them instead, as chunks of a batch do (give both, and the batch's n_tokens); dw_head is then float32 also where
+    only `loss` is given."""
     T, H = hidden.shape
     V = w_head.shape[0]
     dt = _dtype_code(hidden)
@@ -652,7 +653,8 @@ def distill_loss(hidden: torch.Tensor, w_head: torch.Tensor, teacher_ids: torch.
                  status: Optional[torch.Tensor] = None):
     """Distillation from a teacher's top K logits per token, with its gradient: (loss [1] f64, token_loss [T]
     f32, lse [T] f32, dhidden, dw_head). teacher_ids [T, K] int32 (-1: no entry), teacher_logits [T, K] f32;
-    teacher_lse [T] f32, the teacher's log-sum-exp over its whole vocabulary at `temperature`, or None to
+    teacher_lse [T] f32, the teacher's log-sum-exp over its whole vocabulary at `temperature` (which weighs a token by
+    the probability that its K entries hold: the optimum is the teacher renormalised over them either way), or None to
     normalise over the K. Outputs, accumulation and the other arguments as in cross_entropy."""
     T, H = hidden.shape
     V = w_head.shape[0]

@@ -7,7 +7,8 @@
 //   dx_tj = (coef / N) p_tj [(1 - sigmoid(x_tj))] (f_j - sum_e f_e p_te).
 // f depends on the choices alone, so the logits are read once: the choices are counted first, then one pass
 // forms loss and gradient of each token from registers. Bound by HBM: the logits in, their gradient out.
-// Counts are integer atomics (their order does not show); the loss is summed in float64 in a fixed order.
+// Counts are integer atomics (their order does not show); the loss is summed in float64 in a fixed order. Exponentials
+// and reciprocals are the hardware's, each within a unit of the last place of a float, and take no branches for ranges.
 #include "common.hpp"
 #include "launch.hpp"
 #include "layout.hpp"

@@ -16,8 +16,10 @@
 // the logits themselves never reach memory.
 //
 // Rounding (bf16 operands): the exponentials are kept as fp16, scaled so that a half tile's largest is
-// 2^15: 11 significand bits down to 2^-29 of it, an absolute 2^-39 of it below. dz is rounded once more,
-// to bf16, whose 8 bits dominate; lse and the loss come from the unrounded sums. The mean's 1 / N (and tau)
+// 2^15: 11 significand bits down to 2^-29 of it, an absolute 2^-39 of it below. dz, q's entries and a token's weight
+// within it, is rounded once more, to bf16 as an operand of the matrix instructions, also for a float32 dW: its 8
+// bits dominate (0.0017 of a gradient's norm, as much as a bf16 result's own rounding). lse and the loss come from
+// the unrounded sums. The mean's 1 / N (and tau)
 // multiply the gradients' sums: in dz they would be rounded alike in every token whose p is small against 1,
 // as much as 2^-8 off in all of them. Referring to the half tile's own maximum keeps logits in range without a
 // row maximum known beforehand: of magnitudes up to 1.8e8 (kMaxRef), where float32 logits lie 16 apart; rows whose
@@ -201,9 +203,9 @@ void k_exp_logits(GemmShape s, GemmShape st, EpiExp<E, false, kStore> epi, EpiEx
   }
 }
 
-// The same for few rows, up to 16 NT: bound by reading W once. 1 / 64 / 128 rows of the 2048 x 151,936
-// head (622 MB): 186 / 198 / 256 us, 3.4 TB/s for the first; of 6144 (1867 MB) 390 / 449 / 638, 4.8 TB/s; whole
-// tiles 272 and 650 whatever the rows up to 256. A block takes a half tile, 128 vocabulary
+// The same for few rows, up to 16 NT: bound by reading W once. Of 2048 x 151,936 (622 MB), in calls for dH: 1 / 64 /
+// 128 rows 134 / 159 / 240 us, by whole tiles 64 / 128 / 256 rows 188 / 194 / 204; of 6144 (1867 MB) 342 / 415 / 612, by
+// whole tiles 510 / 520 / 528. (Behind a call that wrote dW, the first takes 186 us: 3.4 TB/s.) A block takes a half tile, 128 vocabulary
 // rows, 32 per wave as two 16-row MFMA operands loaded straight into registers, 256 contiguous bytes of a row per
 // stage, the next stage's on their way during this one's products; the tokens' stage is staged through LDS, twice
 // buffered. Rows lie 2 H bytes apart, a multiple of the memory channels' interleave where H is one of 2048, so
@@ -211,12 +213,11 @@ void k_exp_logits(GemmShape s, GemmShape st, EpiExp<E, false, kStore> epi, EpiEx
 // Four blocks' worth of waves per CU finish at different times, where whole tiles (594 of them for 256 CUs) leave
 // two thirds of the CUs idle in the last round. Also writes the targets' logits (CE), from the accumulators, so
 // that they agree with the terms of the sum. fp32 operands go through the fp32 MFMA, four K at a time: up to 64
-// rows its rate (256 flop/clk/CU) hides under the reads: 1 / 32 / 64 / 65 rows of 2048 x 151,936 (1245 MB) 230 / 264
-// / 434 us, and 742 by whole tiles (bf16, 64 / 128 / 129: 196 / 251 and 264; of 1024 x 50,257, 64 / 65 / 163: 26 / 47 and
-// 40). A short pass takes it for any number of rows, a group of 16 NT per blockIdx.y, where that makes no more
-// than one block per CU: whole tiles would leave most CUs idle, and the tile engine's code takes longer to fetch (163
-// rows of 64 x 1000 in fp32: 9 and 24 us; 512 of 2048 x 8000: 161, and 240 for a tile; bf16: 1024 rows of 2048 x
-// 8000 would be two blocks per CU, 82, against one tile's 50).
+// rows its rate (256 flop/clk/CU) hides under the reads: 1 / 32 / 64 rows of 2048 x 151,936 (1245 MB) 232 / 281 / 449
+// us, 64 by whole tiles 715; of 1024 x 50,257 64 rows 91, 65 by whole tiles 148. A short pass takes it for any number
+// of rows, a group of 16 NT per blockIdx.y, where that makes no more than one block per CU: whole tiles would leave
+// most CUs idle, and the tile engine's code takes longer to fetch (163 rows of 64 x 1000 in fp32: 9.5 and 23 us; 256 of
+// 2048 x 8000 105 and 230; bf16: 512 of 2048 x 8000 45 and 49, where 1024 would be two blocks per CU, 82 against 54).
 constexpr int64_t kFewRows = 64;
 constexpr int64_t kFewBlocks = kGpuCus;
 // Rows that a block of k_exp_logits_few takes in a call of T tokens, and whether such blocks are used.
