@@ -282,7 +282,8 @@ inline ValueLayout value_layout(int64_t T, int64_t H) {
 
 // sao_cross_entropy / sao_distill_loss. Rows that count are compacted and go through the head in
 // chunks of `rows`: a chunk's exponentials (2 bytes a logit for bf16, 4 for fp32) fit kExpBytes, so
-// the workspace does not grow with T beyond that. 5 GiB hold 17,408 rows of a 151,936-row vocabulary
+// that beyond it only what is kept per row grows with T (the compacted rows, their indices and logits at the
+// sparse entries). 5 GiB hold 17,408 rows of a 151,936-row vocabulary
 // in bf16, 68 token tiles; a chunk's weight gradient is then one product over thousands of rows and
 // adding it to the others costs 2 % of the chunk.
 constexpr size_t kExpBytes = size_t{5} << 30;
